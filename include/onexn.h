@@ -305,8 +305,8 @@ onexn_status onexn_fc_fwd(const int32_t* P_dev, const int32_t* I_dev, const void
  *          refused).
  * u_dev:   out, fp32 [rows][r] for the backward call, or NULL.
  * Arrays are aligned to their elements; strides are at least the width.  Sums
- * are fp32; a bf16 layer's second product takes u in bf16 parts that hold 16
- * bits of it for a bf16 y and all 24 for an fp32 y.
+ * are fp32; a bf16 layer's second product takes all 24 bits of u, whatever y's
+ * type is.
  * Where x, u or a factor is not finite, the row's results are not.
  * Supported: 1 <= r <= 128, L <= 32767, rows <= 2^26, m and n <= 2^27, r*m and
  *         r*n below 2^31.

@@ -65,22 +65,17 @@ __device__ __forceinline__ u32x4 without_first(u32x4 w, int32_t skip) {
     return w;
 }
 
-// Planes of eight floats: v is cut to its upper 16 bits, the remainder (exact)
-// likewise, and so on; the last of two planes is rounded, a third holds what
-// is left exactly.  Two planes hold v to 2^-15 of it, three exactly (down to
-// bf16's last subnormal bit, 2^-133).  Cut, unlike rounded, no finite value
-// gets an infinite plane; an infinite one gets NaN in the second.
-template <int P>
-__device__ __forceinline__ void cut_planes(const float (&v)[8], u32x4 (&p)[P]) {
+// The three planes of eight floats: v is cut to its upper 16 bits, the remainder
+// (exact) likewise, and the third holds what is left: v exactly, down to bf16's
+// last subnormal bit, 2^-133.  Cut, unlike rounded, no finite value gets an
+// infinite plane; an infinite one gets NaN in the second.
+constexpr int kPlanes = 3;
+__device__ __forceinline__ void cut_planes(const float (&v)[8], u32x4 (&p)[kPlanes]) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         float a = v[2 * k], b = v[2 * k + 1];
 #pragma unroll
-        for (int t = 0; t < P; ++t) {
-            if (P == 2 && t == 1) {
-                p[t][k] = round_pair(a, b);
-                break;
-            }
+        for (int t = 0; t < kPlanes; ++t) {
             p[t][k] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
             a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
             b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);

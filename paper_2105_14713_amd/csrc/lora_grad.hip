@@ -37,7 +37,7 @@ struct GradArgs {
 
 template <typename T, int RT>
 __global__ void __launch_bounds__(kWaves * 64) lora_grad(const GradArgs a) {
-    constexpr int V = Mat<T>::V, KB = 4 * V, COLS = 16 * V, P = sizeof(T) == 4 ? 1 : 3;
+    constexpr int V = Mat<T>::V, KB = 4 * V, COLS = 16 * V, P = sizeof(T) == 4 ? 1 : kPlanes;
     constexpr int THREADS = kWaves * 64, STEPS = kList / THREADS;
     __shared__ float sPart[kWaves * 16 * COLS];
     __shared__ int32_t sList[kList], sCount[STEPS * kWaves];
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kWaves * 64) lora_grad(const GradArgs a) {
 #pragma unroll
                     for (int e = 0; e < V; ++e) uf[t][0][e] = __float_as_uint(uv[t][e]);
                 } else {
-                    cut_planes<P>(uv[t], uf[t]);
+                    cut_planes(uv[t], uf[t]);
                 }
             }
 #pragma unroll
