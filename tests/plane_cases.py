@@ -8,7 +8,7 @@ the integer, so that the sum that gives u is exact in fp32 in any order.
 """
 import torch
 
-from adapter_reference import NONE
+from adapter_reference import NONE, forward
 
 
 def cut(v, planes):
@@ -27,10 +27,9 @@ def cut_two_rounded(v):
 
 
 def integers(gen, *shape):
-    """24-bit integers with bits in all three planes, either sign."""
-    v = torch.randint(2 ** 22, 2 ** 23, shape, generator=gen) * 2 + 1
-    third = torch.randint(64, 128, shape, generator=gen) * 2 + 1      # odd, 8 bits: the third plane
-    v = (v & ~0xff | third).float()
+    """24-bit integers whose three planes are their three bytes (each with its
+    upper bit, so that none reaches into the next, and the last one odd), either sign."""
+    v = (torch.randint(2 ** 23, 2 ** 24, shape, generator=gen) | 0x008081).float()
     return torch.where(torch.rand(shape, generator=gen) < 0.5, v, -v)
 
 
@@ -102,3 +101,44 @@ def product(T, m, n, r, L, how, dt, odt, seed):
     B, pair = wide_operand(gen, n, r, L, dt)
     scale = (2.0 ** torch.randint(-1, 2, (L,), generator=gen)).float()
     return {"x": x, "A": A, "B": B, "ids": ids, "base": base_of(gen, ids, pair, odt), "scale": scale}
+
+
+def _spread(rows, count):
+    """`count` of these rows (some of them again where there are fewer), over all of them."""
+    return rows[(torch.arange(count) * rows.numel() // count) if rows.numel() > count
+                else torch.arange(count) % rows.numel()]
+
+
+def gradients(T, m, n, r, L, how, dt, seed):
+    """x, A, B, ids, u, dy, scale of a backward call whose dA and dB are single products:
+    each column of an adapter's x is nonzero in one of its rows, and u in one row for each
+    triple of columns that dy selects."""
+    gen = torch.Generator().manual_seed(seed)
+    ids = make_ids(gen, T, L, how)
+    dy, B, pick = narrow_operands(gen, T, n, r, L, dt)
+    x, u = torch.zeros(T, m), torch.zeros(T, r)
+    for l in range(L):
+        rows = (ids == l).nonzero()[:, 0]
+        if not rows.numel():
+            continue
+        sign = torch.where(torch.rand(m, generator=gen) < 0.5, 1.0, -1.0)
+        x[_spread(rows, m), torch.arange(m)] = sign
+        for k in pick[rows].unique():
+            at = rows[pick[rows] == k]
+            u[at[int(torch.randint(0, at.numel(), (1,), generator=gen))]] = integers(gen, r)
+    scale = (2.0 ** torch.randint(-1, 2, (L,), generator=gen)).float()
+    return {"x": x.to(dt), "A": torch.zeros(L, r, m, dtype=dt), "B": B, "ids": ids, "u": u, "dy": dy, "scale": scale}
+
+
+def factor_gradients(c, keep=None):
+    """(dA, dB) of such a case in float64, with u and g held as `keep` gives them."""
+    g, _ = forward(c["dy"], c["B"], c["A"], c["ids"], None, c["scale"])
+    u = c["u"].double()
+    if keep is not None:
+        g, u = keep(g.float()).double(), keep(c["u"]).double()
+    dA = torch.zeros(c["A"].shape, dtype=torch.float64)
+    dB = torch.zeros(c["B"].shape, dtype=torch.float64)
+    for l in range(dA.shape[0]):
+        at = c["ids"] == l
+        dA[l], dB[l] = g[at].t() @ c["x"][at].double(), u[at].t() @ c["dy"][at].double()
+    return dA, dB

@@ -8,8 +8,8 @@ import plane_cases
 from adapter_reference import forward
 
 F32, BF16 = torch.float32, torch.bfloat16
-TYPES = [(BF16, BF16)]
-TYPE_IDS = ["bf16"]
+TYPES = [(BF16, BF16), (BF16, F32), (F32, F32)]
+TYPE_IDS = ["bf16", "bf16_yf32", "f32"]
 
 CASES = [  # T, m, n, r, L, how: each rank class in each way that rows are put into tiles
     (1, 40, 50, 2, 1, "mixed"), (33, 200, 168, 2, 3, "mixed"), (40, 200, 168, 16, 3, "mixed"),
@@ -86,3 +86,41 @@ def test_every_bit_of_g(case, types):
     dx, _, _ = onexn.fc_lora_bwd(None, d["B"], d["A"], d["ids"], None, d["x"], d["base"], d["scale"],
                                  need=(True, False, False))
     assert torch.equal(dx.cpu(), ref.to(types[1]))
+
+
+GRADIENTS = [  # T, m, n, r, L, how: each rank class of the gradients' kernel, one range of rows and several
+    (1, 40, 50, 2, 1, "runs"), (60, 200, 168, 9, 3, "mixed"), (60, 129, 131, 30, 3, "mixed"),
+    (300, 96, 200, 64, 4, "mixed"), (300, 130, 90, 101, 2, "runs"), (1024, 72, 136, 16, 2, "mixed"),
+    (1100, 72, 136, 16, 2, "mixed"), (3000, 256, 264, 32, 3, "runs"), (3000, 136, 72, 48, 1, "mixed"),
+    (5000, 72, 80, 128, 2, "mixed"), (300, 40, 48, 4, 60, "mixed"), (30, 7, 6, 3, 2, "mixed"),
+]
+GRADIENT_IDS = ["x".join(map(str, c)) for c in GRADIENTS]
+
+
+@pytest.mark.parametrize("case", GRADIENTS, ids=GRADIENT_IDS)
+def test_gradients_of_fewer_planes_would_not_pass(case):
+    c = plane_cases.gradients(*case, BF16, sum(case[:5]))
+    ref = plane_cases.factor_gradients(c)
+    used = torch.tensor([bool((c["ids"] == l).any()) for l in range(case[4])])
+    for keep, name in SHORT:
+        # (g of a second rank of a pair has 16 bits: the first ranks differ, in every column of x;
+        # u has 24, in every column of a triple that a row selects.)
+        dA, dB = plane_cases.factor_gradients(c, keep)
+        assert ((dA != ref[0])[:, ::2].all(2).all(1) == used).all(), name
+        assert ((dB != ref[1]) == (ref[1] != 0)).all() and (dB != ref[1]).flatten(1).any(1).equal(used), name
+    for a, b in zip(plane_cases.factor_gradients(c, lambda v: plane_cases.cut(v, 3)), ref):
+        assert torch.equal(a, b) and torch.equal(b.float().double(), b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", GRADIENTS, ids=GRADIENT_IDS)
+def test_every_bit_of_the_gradients(case, dt):
+    print("lora planes, gradients", case, dt, flush=True)
+    c = plane_cases.gradients(*case, dt, sum(case[:5]))
+    ref = plane_cases.factor_gradients(c)
+    d = {k: v.cuda() for k, v in c.items()}
+    _, dA, dB = onexn.fc_lora_bwd(d["x"], d["A"], d["B"], d["ids"], d["u"], d["dy"], None, d["scale"],
+                                  need=(False, True, True))
+    assert torch.equal(dA.cpu().double(), ref[0])
+    assert torch.equal(dB.cpu().double(), ref[1])
