@@ -367,10 +367,13 @@ onexn_status onexn_fc_lora_bwd(const void* x_dev, onexn_dtype xdt, int64_t x_str
  *          c = 1; out[k] may be grads[k].  No tensor may overlap another one
  *          of the list (nor be listed twice), or another one's output.
  * max_norm: positive and finite.  norm_dev: out, device fp32: N of the
- *          gradients before clipping; may be NULL for onexn_clip_grads.
- * Squares are summed in 64 bits in a fixed order.  c * g is rounded once, to
- * the gradient's type.  An infinite N gives c = 0 (and NaN for infinite
- * gradients), a NaN makes all of them NaN: look at the norm before a step.
+ *          gradients before clipping (infinite where N is beyond fp32); may be
+ *          NULL for onexn_clip_grads.
+ * Squares are summed in 64 bits in a fixed order; N, c and c * g are 64-bit,
+ * so finite gradients are clipped to any max_norm, whatever their size.  c * g
+ * is rounded to fp32, and for bf16 gradients from there to bf16.  Infinite
+ * gradients give c = 0 (and NaN for themselves), a NaN makes all of them NaN:
+ * look at the norm before a step.
  * workspace_dev: at least onexn_grad_workspace_bytes(count) bytes, 8-byte
  *          aligned, nothing in it needs initialising; not to be used otherwise
  *          until the work enqueued here has finished.
