@@ -289,6 +289,7 @@ __device__ __forceinline__ void rows_pass(const LoraRowsArgs& a, const Rows rows
             }
         }
     const bool in_place = a.y == a.base && a.y_stride == a.base_stride;
+    const float none = a.base ? -0.f : 0.f;      // what changes no base, -0 neither
     for (; ch < chunk1; ch += W) {
         const int32_t col = column_of(ch), skip = min((ch * 16 + n16) * V - col, V);
         at = first;
@@ -298,7 +299,11 @@ __device__ __forceinline__ void rows_pass(const LoraRowsArgs& a, const Rows rows
             const bool last = !at.left;
             if (last) at = first;
             else at.next();
-            f32x4 acc[NT][V] = {};
+            f32x4 acc[NT][V];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[t][i] = l >= 0 ? f32x4{0, 0, 0, 0} : f32x4{none, none, none, none};
             if (l >= 0) {
 #pragma unroll
                 for (int set = 0; set < SETS; ++set) {
@@ -524,7 +529,7 @@ __global__ void __launch_bounds__(kThreads) lora_rows_small(const LoraRowsArgs a
         }
         __syncthreads();
         for (int32_t o = threadIdx.x; a.y && o < a.n; o += kThreads) {
-            float s = 0;
+            float s = l < 0 && a.base ? -0.f : 0.f;     // (as in rows_pass)
             if (l >= 0) {
                 const T* w = static_cast<const T*>(a.W2) + int64_t(l) * a.r * a.n + o;
                 for (int32_t j = 0; j < a.r; ++j) s = fmaf(u[j], to_f32(w[int64_t(j) * a.n]), s);
