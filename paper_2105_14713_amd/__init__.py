@@ -548,6 +548,13 @@ def fc_lora_bwd(x: Optional[torch.Tensor], A: torch.Tensor, B: torch.Tensor, ids
     return out if need_dx else None, dA if need_dA else None, dB if need_dB else None
 
 
+def _same_layout(a, b):
+    """Whether two tensors of one shape have each element at the same offset (a
+    dimension of one element may have any stride: [n][m][1][1] is the same in
+    both memory formats)."""
+    return a.numel() == 0 or all(n == 1 or s == t for n, s, t in zip(a.shape, a.stride(), b.stride()))
+
+
 class BoundGrads:
     """A list of gradients, and of the tensors that take them clipped (``out``;
     without it they are clipped in place), validated and marshalled once for
@@ -574,7 +581,7 @@ class BoundGrads:
             spans.append((g.data_ptr(), g.numel() * g.element_size()))
             if out is not None:
                 o = out[i]
-                if o.shape != g.shape or o.stride() != g.stride() or o.dtype != g.dtype or \
+                if o.shape != g.shape or not _same_layout(o, g) or o.dtype != g.dtype or \
                         o.get_device() != self.device:
                     raise ValueError(f"out {i} has the wrong shape, dtype, layout or device")
                 if o.data_ptr() != g.data_ptr():
