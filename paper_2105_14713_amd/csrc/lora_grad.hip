@@ -160,17 +160,54 @@ __global__ void __launch_bounds__(kWaves * 64) lora_grad(const GradArgs a) {
     }
 }
 
-// Any size: a column a thread, every row looked at.
+// Fewer columns than a lane's 16 bytes hold (job[0] alone): one rank of one adapter
+// and a range of rows a workgroup, a row a thread, up to V - 1 sums each, which
+// meet in lane, wave and range order (8192 rows of two bf16 columns, rank 16: 11
+// us; a thread a column that goes through all rows: 1.1 ms, and one fp32 sum of
+// all of them).  Each factor goes by its own width: the other one, 4096 wide, takes
+// 39 us with lora_grad.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) lora_grad_small(const Job job, const int32_t* __restrict__ ids,
-                                                            int32_t rows, int32_t r) {
-    const int32_t c = blockIdx.x * kThreads + threadIdx.x, j = blockIdx.z, l = blockIdx.y;
-    if (c >= job.C) return;
-    float s = 0;
-    for (int32_t i = 0; i < rows; ++i)
-        if (ids[i] == l)
-            s = fmaf(job.u[int64_t(i) * r + j], to_f32(static_cast<const T*>(job.v)[i * job.v_stride + c]), s);
-    job.out[(int64_t(l) * r + j) * job.C + c] = s;
+__global__ void __launch_bounds__(kWaves * 64) lora_grad_small(const GradArgs a) {
+    constexpr int MOST = Mat<T>::V - 1;
+    __shared__ float sPart[kWaves][MOST];
+    __shared__ int32_t sFound[kWaves];
+    const Job& job = a.job[0];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int32_t j = blockIdx.x, l = blockIdx.y;
+    const int32_t begin = blockIdx.z * a.range, end = min(begin + a.range, a.rows);
+    float s[MOST] = {};
+    bool mine = false;
+    for (int32_t i = begin + int32_t(threadIdx.x); i < end; i += kWaves * 64) {
+        if (a.ids[i] != l) continue;
+        mine = true;
+        const float u = job.u[int64_t(i) * a.r + j];
+        const T* const v = static_cast<const T*>(job.v) + i * job.v_stride;
+#pragma unroll
+        for (int c = 0; c < MOST; ++c)
+            if (c < job.C) s[c] = fmaf(u, to_f32(v[c]), s[c]);
+    }
+    const uint64_t any = __ballot(mine);
+#pragma unroll
+    for (int c = 0; c < MOST; ++c) {
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) s[c] += __shfl_xor(s[c], d);
+        if (lane == 0) sPart[wave][c] = s[c];
+    }
+    if (lane == 0) sFound[wave] = any != 0;
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c < job.C) {
+        float sum = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += sPart[w][c];
+        job.out[((int64_t(blockIdx.z) * a.L + l) * a.r + j) * job.C + c] = sum;
+    }
+    if (gridDim.z > 1 && j == 0 && threadIdx.x == 0) {
+        int32_t found = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) found |= sFound[w];
+        a.present[int64_t(blockIdx.z) * a.L + l] = found;
+    }
 }
 
 struct JoinArgs {
@@ -259,33 +296,33 @@ void launch_lora_grad(const LoraGradArgs& g, onexn_dtype dt, hipStream_t s) {
     join.present = a.present;
     join.L = g.L;
     join.splits = splits;
-    int jobs = 0;
+    int wide = 0, joined = 0;
     for (int k = 0; k < 2; ++k) {
         float* dW = k ? g.dB : g.dA;
         if (!dW) continue;
         const int32_t C = k ? g.n : g.m;
         const int64_t size = int64_t(g.L) * g.r * C;
-        a.job[jobs] = {k ? g.u : g.g, k ? g.dy : g.x, splits > 1 ? part : dW, k ? g.dy_stride : g.x_stride, C,
-                       (C + cols - 1) / cols};
-        join.part[jobs] = part;
-        join.dW[jobs] = dW;
-        join.size[jobs] = size;
-        join.adapter[jobs] = int64_t(g.r) * C;
-        part += size * splits;
-        ++jobs;
-    }
-    if (g.m < 8 || g.n < 8) {        // (a row holds less than a lane's 16 bytes)
-        for (int k = 0; k < jobs; ++k) {
-            a.job[k].out = join.dW[k];
-            const dim3 grid((a.job[k].C + kThreads - 1) / kThreads, g.L, g.r), block(kThreads);
-            if (dt == ONEXN_F32) hipLaunchKernelGGL(lora_grad_small<float>, grid, block, 0, s, a.job[k], g.ids, g.rows, g.r);
-            else hipLaunchKernelGGL(lora_grad_small<uint16_t>, grid, block, 0, s, a.job[k], g.ids, g.rows, g.r);
+        const Job job{k ? g.u : g.g, k ? g.dy : g.x, splits > 1 ? part : dW, k ? g.dy_stride : g.x_stride, C,
+                      (C + cols - 1) / cols};
+        if (C >= (dt == ONEXN_F32 ? Mat<float>::V : Mat<uint16_t>::V)) {
+            a.job[wide++] = job;
+        } else {                         // (a row holds less than a lane's 16 bytes)
+            GradArgs narrow = a;
+            narrow.job[0] = job;
+            const dim3 grid(g.r, g.L, splits), block(kWaves * 64);
+            if (dt == ONEXN_F32) hipLaunchKernelGGL(lora_grad_small<float>, grid, block, 0, s, narrow);
+            else hipLaunchKernelGGL(lora_grad_small<uint16_t>, grid, block, 0, s, narrow);
         }
-        return;
+        join.part[joined] = part;
+        join.dW[joined] = dW;
+        join.size[joined] = size;
+        join.adapter[joined] = int64_t(g.r) * C;
+        part += size * splits;
+        ++joined;
     }
     const dim3 grid(a.job[0].chunks + a.job[1].chunks, g.L, splits);
-    if (dt == ONEXN_F32) launch_grad<float>(a, grid, s);
-    else launch_grad<uint16_t>(a, grid, s);
+    if (wide && dt == ONEXN_F32) launch_grad<float>(a, grid, s);
+    else if (wide) launch_grad<uint16_t>(a, grid, s);
     if (splits > 1) {
         const int64_t blocks = (join.size[0] + join.size[1] + kThreads - 1) / kThreads;
         hipLaunchKernelGGL(lora_grad_join, dim3(uint32_t(blocks < 4096 ? blocks : 4096)), dim3(kThreads), 0, s, join);

@@ -1,0 +1,83 @@
+"""The factors' gradients of layers with few columns on one side (a head of a few
+classes, a narrow input): each factor by its own width, sums over many rows."""
+import pytest
+import torch
+
+import paper_2105_14713_amd as onexn
+from adapter_reference import backward, backward_bounds
+from test_gpu_fc_lora import BF16, F32, TYPE_IDS, TYPES, check_exact, make, run_fwd
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    onexn.load_library()
+
+
+@pytest.mark.parametrize("types", TYPES, ids=TYPE_IDS)
+@pytest.mark.parametrize("m,n", [(200, 2), (200, 7), (3, 200), (5, 2), (4, 4), (7, 8), (1, 1), (8, 1), (600, 5)])
+@pytest.mark.parametrize("T,r,L,how", [(40, 5, 3, "mixed"), (1024, 16, 1, "runs"), (1025, 33, 2, "mixed"),
+                                       (5000, 70, 4, "runs"), (3000, 4, 40, "mixed"), (9000, 8, 1, "mixed"),
+                                       (2000, 3, 2, "none")])
+def test_integer_exact(T, r, L, how, m, n, types):
+    check_exact(make(T, m, n, r, L, how, *types, True, T + m + n), f"lora narrow {T} {m}x{n} rank {r} {L} {how} {types}")
+
+
+@pytest.mark.parametrize("types", TYPES, ids=TYPE_IDS)
+@pytest.mark.parametrize("T,m,n,r,L", [(700, 300, 2, 9, 2), (6000, 300, 3, 16, 2), (6000, 6, 300, 16, 1)])
+def test_random_within_bounds(T, m, n, r, L, types):
+    print("lora narrow random", T, m, n, r, L, types, flush=True)
+    c = make(T, m, n, r, L, "mixed", *types, False, 3)
+    u, _, d = run_fwd(c)
+    out = onexn.fc_lora_bwd(d["x"], d["A"], d["B"], d["ids"], u, d["dy"], d["dbase"], d["scale"])
+    args = (c["x"], c["A"], c["B"], c["ids"], c["dy"], c["dbase"], c["scale"])
+    for got, ref, e in zip(out, backward(*args), backward_bounds(*args, types[1])):
+        assert ((got.cpu().double() - ref).abs() <= e).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("need", [(False, True, False), (False, False, True), (False, True, True)])
+@pytest.mark.parametrize("T", [600, 3000])
+def test_one_factor_alone_rows_apart_and_poison(T, need, dt):
+    """Rows of other adapters and without one are not read, what lies behind the rows neither."""
+    print("lora narrow parts", T, need, dt, flush=True)
+    c = make(T, 90, 3, 6, 3, "mixed", dt, dt, True, T)
+    none = (c["ids"] < 0) | (c["ids"] >= 3)
+    ref = backward(c["x"], c["A"], c["B"], c["ids"], c["dy"], None, c["scale"])
+    u, _, _ = run_fwd(c)
+    u[none.cuda()] = float("nan")
+    wide_x = torch.full((T, 97), float("nan"), dtype=dt)
+    wide_dy = torch.full((T, 11), float("nan"), dtype=dt)
+    wide_x[:, 2:92], wide_dy[:, 5:8] = c["x"], c["dy"]
+    wide_x[none], wide_dy[none] = float("nan"), float("inf")
+    _, dA, dB = onexn.fc_lora_bwd(wide_x.cuda()[:, 2:92], c["A"].cuda(), c["B"].cuda(), c["ids"].cuda(), u,
+                                  wide_dy.cuda()[:, 5:8], None, c["scale"].cuda(), need=need)
+    if need[1]:
+        assert torch.equal(dA.cpu().double(), ref[1])
+    if need[2]:
+        assert torch.equal(dB.cpu().double(), ref[2])
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_long_sums(dt):
+    """2^24 + 1000 ones: one fp32 sum after the other stays at 2^24."""
+    T, m, n = 2 ** 24 + 1000, 8, 2
+    print("lora narrow long", dt, flush=True)
+    x, dy = torch.ones(T, m, dtype=dt, device="cuda"), torch.ones(T, n, dtype=dt, device="cuda")
+    ids, u = torch.zeros(T, dtype=torch.int32, device="cuda"), torch.ones(T, 1, device="cuda")
+    A, B = torch.ones(1, 1, m, dtype=dt, device="cuda"), torch.tensor([[[1.0, 0.0]]], dtype=dt, device="cuda")
+    _, dA, dB = onexn.fc_lora_bwd(x, A, B, ids, u, dy, need=(False, True, True))
+    assert (dA == float(T)).all() and (dB == float(T)).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_results_do_not_vary(dt):
+    c = make(5000, 130, 3, 12, 2, "mixed", dt, dt, False, 4)
+    u, _, d = run_fwd(c)
+    first = onexn.fc_lora_bwd(d["x"], d["A"], d["B"], d["ids"], u, d["dy"], d["dbase"], d["scale"])
+    for _ in range(3):
+        again = onexn.fc_lora_bwd(d["x"], d["A"], d["B"], d["ids"], u, d["dy"], d["dbase"], d["scale"])
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
