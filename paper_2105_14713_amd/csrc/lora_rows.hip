@@ -577,13 +577,18 @@ void launch(const LoraRowsArgs& a, hipStream_t s) {
     }
     // Tiles of 32 rows read the factors half as often, which counts from rank 33
     // on where there is a tile for every CU (16384 rows, 4096 -> 8192, r = 64: 175
-    // us against 195; r = 16, 8192 rows: 44 against 43).
+    // us against 195; r = 16, 8192 rows: 44 against 43).  Above rank 64 one tile of 16
+    // takes all 256 registers already.
     if constexpr (RT == 4)
         if (a.rows >= 8192) return launch_run<T, TY, RT, 2, kWaves>(a, s);
-    // Narrow layers have no work for eight waves in either product (bf16, 20000
-    // rows, 256 -> 512, r = 16: 10.7 us with four, 13.6 with eight; 8192 rows of
-    // 512: 6.7 and 6.8, of 256 -> 1024: 9.1 and 8.3).
-    if (a.m <= 4 * 16 * Mat<T>::V && a.n <= 4 * 16 * Mat<T>::V) return launch_run<T, TY, RT, 1, 4>(a, s);
+    // Narrow layers have no work for eight waves in either product, and where tiles
+    // wait for a CU, workgroups of four come in sooner: from 4097 rows on four waves
+    // are as fast or faster at every rank (64 to 512 columns; 8192 rows of 256, r =
+    // 16: 5.6 us against 6.0, r = 128: 10.7 and 14.7; 20000 rows 7.8 and 10.8), up to
+    // 4096 rows as fast or slower (r = 128: up to 4 %).  Wider: 8192 rows of 256 ->
+    // 1024, 9.1 and 8.3.
+    if (a.rows > 16 * 256 && a.m <= 4 * 16 * Mat<T>::V && a.n <= 4 * 16 * Mat<T>::V)
+        return launch_run<T, TY, RT, 1, 4>(a, s);
     launch_run<T, TY, RT, 1, kWaves>(a, s);
 }
 

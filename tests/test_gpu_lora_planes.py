@@ -22,7 +22,8 @@ CASES = [  # T, m, n, r, L, how: each rank class in each way that rows are put i
     (50, 200, 168, 96, 1, "mixed"),
     (4200, 96, 104, 16, 5, "mixed"), (4200, 96, 104, 32, 5, "runs"), (4200, 600, 104, 50, 3, "runs"),
     (4200, 96, 104, 70, 2, "runs"), (8200, 64, 72, 40, 1, "mixed"), (8200, 64, 72, 64, 3, "runs"),
-    (30, 7, 6, 3, 2, "mixed"),
+    (4200, 200, 168, 9, 1, "mixed"), (4200, 72, 80, 63, 1, "mixed"), (4200, 80, 72, 50, 2, "runs"),
+    (4200, 72, 80, 100, 1, "mixed"), (30, 7, 6, 3, 2, "mixed"),
 ]
 IDS = ["x".join(map(str, c)) for c in CASES]
 
