@@ -18,7 +18,7 @@
 namespace onexn {
 namespace {
 
-constexpr int kWaves = 8, kList = 2048;
+constexpr int kWaves = 8, kList = 2048, kMostRanks = 64;     // ranks of a workgroup at most
 
 struct Job {
     const float* u;      // [rows][r]
@@ -239,26 +239,33 @@ __global__ void __launch_bounds__(kThreads) lora_grad_join(const JoinArgs a) {
     }
 }
 
-// Ranges of rows, for workgroups enough: with few columns many, with many columns
-// a few for up to eight adapters (most of whose workgroups find no rows in a
-// range where requests stand together).  Up to 1024 rows one range takes as
-// long as four and the second launch that joins them (fp32, 2048 and 1000
-// columns, r = 8: 11.6 us against 7.1 + 2.3 and the launch; 4096 rows of 1024
-// columns, bf16: 16 ranges 9 + 4 us, 4 ranges 10.7 + 4).  Narrow layers leave room
-// for more ranges beside their adapters, taken where that at least doubles them
-// (16384 rows of 256 columns, 16 adapters: one range 33.5 us, eight 14.3 + 4;
-// but 2051 rows of 1023 and 2047 columns, four: four ranges 14.4 us, five 18.4).
-constexpr int kOneRange = 1024, kSplitRows = 256, kSplitMost = 16, kGroups = 512;
+// Ranges of rows, a power of two of them.  From 640 rows an adapter on (with fewer
+// the join's launch costs what they save), each of 128 rows or more, while a CU is
+// left for each workgroup that works: how rows fall to adapters is not known here,
+// and of L adapters a range is taken to hold sqrt(L) (requests one behind the other:
+// one or two; any order: all).  Not two ranges for several adapters: half of the
+// workgroups then have no rows, in blocks that put the others on the same CUs.  Over
+// 2084 calls (some 300 layers of 2 to 8192 columns, r = 2 to 128, one to 16 adapters in
+// runs of equal and of random lengths and in any order, 256 to 16384 rows, both types)
+// this takes 2.6 % longer on average than the best of 1, 2, 4, 8 and 16 ranges of each,
+// 70 % at most; with two ranges 2.9 %, one range always 22 % (at most seven times as
+// long).  Both sides (us, with the rows' kernel): fp32, 1024 rows, 2048 and 1000
+// columns, r = 8: one range 15.8, four 13.1; bf16, 512 rows of 256, r = 16: one 10.2,
+// four 10.9; fp32, 16384 rows of 1023 and 2047, r = 24, four adapters of as many rows:
+// one 101, two 155, four 152, eight 113; of one adapter, bf16, 4096 rows: one 48, four
+// 27, eight 25, sixteen 32.
+constexpr int kCUs = 256, kSplitRows = 640, kRangeRows = 128, kMostRanges = 16;
 
-int32_t splits_of(int32_t rows, int32_t m, int32_t n, int32_t L) {
-    if (rows <= kOneRange) return 1;
-    const int64_t chunks = (int64_t(m) + 127) / 128 + (int64_t(n) + 127) / 128;
-    int64_t s = kGroups / chunks < kSplitMost / L ? kGroups / chunks : kSplitMost / L;
-    const int64_t room = kGroups / (chunks * L);
-    if (room >= 2 * (s < 1 ? 1 : s)) s = room;
-    if (s > kSplitMost) s = kSplitMost;
-    if (s > rows / kSplitRows) s = rows / kSplitRows;
-    return s < 1 ? 1 : int32_t(s);
+// (The workspace is sized for bf16, whose workgroups have more columns.)
+int32_t splits_of(int32_t rows, int32_t m, int32_t n, int32_t r, int32_t L, int32_t cols) {
+    if (rows / L < kSplitRows) return 1;
+    const int64_t chunks = (int64_t(m) + cols - 1) / cols + (int64_t(n) + cols - 1) / cols;
+    const int64_t groups = chunks * ((r + kMostRanks - 1) / kMostRanks);     // of workgroups, a range's
+    int32_t s = 1;
+    while (2 * s <= kMostRanges && rows >= 2 * s * kRangeRows && 2 * s * groups <= kCUs &&
+           (2 * s * groups) * (2 * s * groups) * L <= int64_t(kCUs) * kCUs)
+        s *= 2;
+    return s == 2 && L > 1 ? 4 : s;
 }
 
 size_t round16(size_t v) { return (v + 15) / 16 * 16; }
@@ -266,7 +273,7 @@ size_t round16(size_t v) { return (v + 15) / 16 * 16; }
 }  // namespace
 
 size_t lora_grad_workspace(int32_t rows, int32_t m, int32_t n, int32_t r, int32_t L) {
-    const size_t s = splits_of(rows, m, n, L);
+    const size_t s = splits_of(rows, m, n, r, L, 16 * Mat<uint16_t>::V);
     return s == 1 ? 0 : round16(s * L * r * (size_t(m) + n) * 4) + round16(s * L * 4);
 }
 
@@ -276,13 +283,14 @@ static void launch_grad(const GradArgs& a, dim3 grid, hipStream_t s) {
     if (a.r <= 16) hipLaunchKernelGGL((lora_grad<T, 1>), grid, block, 0, s, a);
     else if (a.r <= 32) hipLaunchKernelGGL((lora_grad<T, 2>), grid, block, 0, s, a);
     else {
-        grid.y *= (a.r + 63) / 64;
+        grid.y *= (a.r + kMostRanks - 1) / kMostRanks;
         hipLaunchKernelGGL((lora_grad<T, 4>), grid, block, 0, s, a);
     }
 }
 
 void launch_lora_grad(const LoraGradArgs& g, onexn_dtype dt, hipStream_t s) {
-    const int32_t splits = splits_of(g.rows, g.m, g.n, g.L), cols = dt == ONEXN_F32 ? 64 : 128;
+    const int32_t cols = 16 * (dt == ONEXN_F32 ? Mat<float>::V : Mat<uint16_t>::V);
+    const int32_t splits = splits_of(g.rows, g.m, g.n, g.r, g.L, cols);
     GradArgs a{};
     JoinArgs join{};
     float* part = static_cast<float*>(g.workspace);

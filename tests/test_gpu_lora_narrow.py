@@ -81,3 +81,20 @@ def test_results_do_not_vary(dt):
     for _ in range(3):
         again = onexn.fc_lora_bwd(d["x"], d["A"], d["B"], d["ids"], u, d["dy"], d["dbase"], d["scale"])
         assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,m,n,r,L", [(639, 64, 64, 8, 1), (640, 64, 64, 8, 1), (1300, 130, 70, 20, 2), (2600, 64, 40, 128, 1),
+                                       (6000, 300, 3, 16, 3), (9000, 2, 3, 5, 1), (5000, 1023, 2047, 24, 1),
+                                       (5200, 200, 300, 4, 8)])
+def test_workspace_is_enough(T, m, n, r, L, dt):
+    """Exactly the bytes that are asked for, for any number of ranges of rows; what lies behind stays."""
+    print("lora workspace", T, m, n, r, L, dt, flush=True)
+    c = make(T, m, n, r, L, "runs", dt, dt, True, T)
+    u, _, d = run_fwd(c)
+    need = onexn.fc_lora_bwd_workspace_bytes(T, m, n, r, L)
+    flat = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    got = onexn.fc_lora_bwd(d["x"], d["A"], d["B"], d["ids"], u, d["dy"], d["dbase"], d["scale"], workspace=flat[:need])
+    for a, b in zip(got, backward(c["x"], c["A"], c["B"], c["ids"], c["dy"], c["dbase"], c["scale"])):
+        assert torch.equal(a.cpu().double(), b.to(a.dtype).double())
+    assert (flat[need:] == 0x5A).all()
