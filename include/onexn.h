@@ -301,9 +301,9 @@ onexn_status onexn_fc_fwd(const int32_t* P_dev, const int32_t* I_dev, const void
  * base_dev: [rows][n] in ydt, rows base_stride apart (the layer's output), or
  *          NULL for 0.  y_dev: [rows][n] in ydt (xdt or F32), rows y_stride
  *          apart; every element of these rows is written.  y may be base
- *          itself (same stride), and must not overlap anything else (y == x is
- *          refused).
- * u_dev:   out, fp32 [rows][r] for the backward call, or NULL.
+ *          itself (same stride), and must not overlap anything else.
+ * u_dev:   out, fp32 [rows][r] for the backward call, or NULL; must not overlap
+ *          anything else.
  * Arrays are aligned to their elements; strides are at least the width.  Sums
  * are fp32; a bf16 layer's second product takes all 24 bits of u, whatever y's
  * type is.
@@ -330,9 +330,9 @@ onexn_status onexn_fc_lora_fwd(const void* x_dev, onexn_dtype xdt, int64_t x_str
  * base_dev, dx_dev: [rows][m] in dxdt (xdt or F32): the input gradient to add
  *          to (the pruned layer's, from onexn_conv2d_bwd_data with kh = kw = H
  *          = W = 1; or NULL for 0) and the sum; dx may be base itself, and must
- *          not overlap anything else (dx == dy or x is refused).
+ *          not overlap anything else.
  * dA_dev, dB_dev: out, fp32 [L][r][m] and [L][r][n]; every element is written
- *          (0 for adapters without rows).
+ *          (0 for adapters without rows).  They must not overlap anything else.
  * Any of dx, dA and dB may be NULL when it is not wanted (not all of them); x
  * is needed for dA, u for dB only.  Rows without an adapter give dx = base and
  * add to no gradient, whatever x, u and dy hold there.

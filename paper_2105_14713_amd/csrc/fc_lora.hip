@@ -14,6 +14,8 @@
 // same two kernels with the factors exchanged: lora_rows.hip (narrow product,
 // then wide product) and lora_grad.hip (a factor's gradient).  Here: the entry
 // points and their checks.
+#include <initializer_list>
+
 #include "lora.h"
 
 namespace onexn {
@@ -64,12 +66,17 @@ onexn_status check_rows(const char* fn, const char* name, const void* p, bool re
     return ONEXN_OK;
 }
 
-// The result may be its base, row for row, and nothing else that the call reads.
-onexn_status check_result(const char* fn, const char* name, const void* y, int64_t stride, const void* base,
-                          int64_t base_stride, const void* in, const void* other) {
-    if (!y) return ONEXN_OK;
-    if (y == in || y == other) return fail(ONEXN_ERR_ARG, "%s: %s must not overlap the inputs", fn, name);
-    if (y == base && stride != base_stride)
+// An output of the call is none of its other arrays (as far as their addresses show it).
+onexn_status check_apart(const char* fn, const char* name, const void* out, std::initializer_list<const void*> others) {
+    for (const void* o : others)
+        if (out && out == o) return fail(ONEXN_ERR_ARG, "%s: %s must not overlap another array", fn, name);
+    return ONEXN_OK;
+}
+
+// The result may be its base, row for row.
+onexn_status check_in_place(const char* fn, const char* name, const void* y, int64_t stride, const void* base,
+                            int64_t base_stride) {
+    if (y && y == base && stride != base_stride)
         return fail(ONEXN_ERR_ARG, "%s: %s is its base, with another row stride", fn, name);
     return ONEXN_OK;
 }
@@ -92,7 +99,9 @@ extern "C" onexn_status onexn_fc_lora_fwd(const void* x_dev, onexn_dtype xdt, in
     if (onexn_status st = check_rows(fn, "y", y_dev, true, ydt, rows, n, y_stride)) return st;
     if (onexn_status st = check_rows(fn, "u", u_dev, false, ONEXN_F32, rows, r, r)) return st;
     if (rows == 0) return ONEXN_OK;
-    if (onexn_status st = check_result(fn, "y", y_dev, y_stride, base_dev, base_stride, x_dev, u_dev)) return st;
+    if (onexn_status st = check_apart(fn, "y", y_dev, {x_dev, A_dev, B_dev, ids_dev, scale_dev, u_dev})) return st;
+    if (onexn_status st = check_apart(fn, "u", u_dev, {x_dev, A_dev, B_dev, ids_dev, scale_dev, base_dev})) return st;
+    if (onexn_status st = check_in_place(fn, "y", y_dev, y_stride, base_dev, base_stride)) return st;
     const LoraRowsArgs a{x_dev, A_dev, B_dev, base_dev, y_dev, u_dev, scale_dev, ids_dev,
                      x_stride, base_stride, y_stride, rows, m, n, r, L};
     launch_lora_rows(a, xdt, ydt, static_cast<hipStream_t>(stream));
@@ -122,8 +131,14 @@ extern "C" onexn_status onexn_fc_lora_bwd(const void* x_dev, onexn_dtype xdt, in
     if (onexn_status st = check_rows(fn, "dx", dx_dev, false, dxdt, rows, m, dx_stride)) return st;
     if (misaligned(dA_dev, 4) || misaligned(dB_dev, 4))
         return fail(ONEXN_ERR_ARG, "%s: dA or dB is not aligned to its elements", fn);
-    if (rows > 0)
-        if (onexn_status st = check_result(fn, "dx", dx_dev, dx_stride, base_dev, base_stride, dy_dev, x_dev)) return st;
+    if (rows > 0) {
+        if (onexn_status st = check_apart(fn, "dx", dx_dev, {x_dev, A_dev, B_dev, ids_dev, scale_dev, u_dev, dy_dev})) return st;
+        if (onexn_status st = check_in_place(fn, "dx", dx_dev, dx_stride, base_dev, base_stride)) return st;
+        if (onexn_status st = check_apart(fn, "dA", dA_dev, {x_dev, A_dev, B_dev, ids_dev, scale_dev, u_dev, dy_dev,
+                                                             base_dev, dx_dev, dB_dev})) return st;
+        if (onexn_status st = check_apart(fn, "dB", dB_dev, {x_dev, A_dev, B_dev, ids_dev, scale_dev, u_dev, dy_dev,
+                                                             base_dev, dx_dev})) return st;
+    }
     const size_t need = onexn_fc_lora_bwd_workspace_bytes(rows, m, n, r, L);
     if (!workspace_dev) return fail(ONEXN_ERR_NULL, "%s: NULL workspace", fn);
     if (workspace_bytes < need)
