@@ -444,6 +444,13 @@ def _exactly(name, t, shape, dtype, device):
     return t.data_ptr()
 
 
+def _check_int32(**sizes):
+    """Sizes that the library takes in 32 bits (ctypes would cut them to that)."""
+    for name, n in sizes.items():
+        if n > 0x7fffffff:
+            raise ValueError(f"{name} = {n} is beyond 32 bits")
+
+
 def _lora_args(v, A, B, ids, scale):
     """Checks what both directions share against the [rows][.] tensor v: returns
     the leading arguments of the library's calls from m to ids, the device, the
@@ -455,6 +462,8 @@ def _lora_args(v, A, B, ids, scale):
         raise ValueError("x must be [rows][m], A [L][r][m] and B [L][r][n]")
     L, r, m = A.shape
     n, rows = B.shape[2], v.shape[0]
+    if (rows | m | n | r | L) >> 31:
+        _check_int32(rows=rows, m=m, n=n, r=r, L=L)
     # (One expression for the usual call; the checks that name what is wrong where it fails.)
     if not (A.dtype is dt and B.dtype is dt and A.get_device() == dev and B.get_device() == dev and
             A.is_contiguous() and B.is_contiguous() and B.shape == (L, r, n) and ids.dtype is torch.int32 and
@@ -501,6 +510,7 @@ def fc_lora_fwd(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, ids: torch.Te
 
 def fc_lora_bwd_workspace_bytes(rows: int, m: int, n: int, r: int, L: int) -> int:
     """``onexn_fc_lora_bwd_workspace_bytes``: device scratch that fc_lora_bwd needs."""
+    _check_int32(rows=rows, m=m, n=n, r=r, L=L)
     return int(load_library().onexn_fc_lora_bwd_workspace_bytes(int(rows), int(m), int(n), int(r), int(L)))
 
 
