@@ -239,32 +239,31 @@ __global__ void __launch_bounds__(kThreads) lora_grad_join(const JoinArgs a) {
     }
 }
 
-// Ranges of rows, a power of two of them.  From 640 rows an adapter on (with fewer
-// the join's launch costs what they save), each of 128 rows or more, while a CU is
-// left for each workgroup that works: how rows fall to adapters is not known here,
-// and of L adapters a range is taken to hold sqrt(L) (requests one behind the other:
-// one or two; any order: all).  Not two ranges for several adapters: half of the
-// workgroups then have no rows, in blocks that put the others on the same CUs.  Over
-// 2084 calls (some 300 layers of 2 to 8192 columns, r = 2 to 128, one to 16 adapters in
-// runs of equal and of random lengths and in any order, 256 to 16384 rows, both types)
-// this takes 2.6 % longer on average than the best of 1, 2, 4, 8 and 16 ranges of each,
-// 70 % at most; with two ranges 2.9 %, one range always 22 % (at most seven times as
-// long).  Both sides (us, with the rows' kernel): fp32, 1024 rows, 2048 and 1000
-// columns, r = 8: one range 15.8, four 13.1; bf16, 512 rows of 256, r = 16: one 10.2,
-// four 10.9; fp32, 16384 rows of 1023 and 2047, r = 24, four adapters of as many rows:
-// one 101, two 155, four 152, eight 113; of one adapter, bf16, 4096 rows: one 48, four
-// 27, eight 25, sixteen 32.
-constexpr int kCUs = 256, kSplitRows = 640, kRangeRows = 128, kMostRanges = 16;
+// Ranges of rows, a power of two of them, joined by a second launch (2.6 us of the
+// host, 2 to 5 of the GPU).  They pay from some 1536 rows of one bf16 adapter at
+// ranks up to 16 on, fewer where a row takes longer (higher ranks, fp32) and more
+// where adapters share the rows; as many, of 128 rows at least, as give one
+// workgroup a CU (three from 10000 rows on).  Not two for several adapters: half of the
+// workgroups then have no rows, in blocks that put the others on the same CUs.
+// Against the best of 1, 2, 4, 8 and 16 ranges of each of 2084 calls (some 300 layers of
+// 2 to 8192 columns, r = 2 to 128, one to 16 adapters in runs of equal and of random
+// lengths and in any order, 256 to 16384 rows, both types) this takes 2.5 % longer on
+// average and 70 % at most; one range always 22 %, at most seven times as long.  Both
+// sides (us): fp32, 16384 rows of 1023 and 2047, r = 24, four adapters of as many rows:
+// one range 101, two 155, four 152, eight 113; one adapter, bf16, 4096 such rows: one 48,
+// four 27, eight 25, sixteen 32.  A step (forward and backward) called from Python,
+// bf16: 1024 rows of 1024, r = 32: one 26.6, four 28.8; 2048 rows: 31.3 and 29.0.
+constexpr int kCUs = 256, kSplitRows = 1536, kLongRows = 10000, kRangeRows = 128, kMostRanges = 16;
 
-// (The workspace is sized for bf16, whose workgroups have more columns.)
-int32_t splits_of(int32_t rows, int32_t m, int32_t n, int32_t r, int32_t L, int32_t cols) {
-    if (rows / L < kSplitRows) return 1;
+int32_t splits_of(int32_t rows, int32_t m, int32_t n, int32_t r, int32_t L, onexn_dtype dt) {
+    const int32_t cols = 16 * (dt == ONEXN_F32 ? Mat<float>::V : Mat<uint16_t>::V);
+    // (A row's cost goes with the root of its ranks and bytes; so does what L adapters share.)
+    const int64_t cost = (r <= 16 ? 1 : r <= 32 ? 2 : 4) * (dt == ONEXN_F32 ? 2 : 1);
+    if (int64_t(rows) * rows * cost < int64_t(kSplitRows) * kSplitRows * L) return 1;
     const int64_t chunks = (int64_t(m) + cols - 1) / cols + (int64_t(n) + cols - 1) / cols;
-    const int64_t groups = chunks * ((r + kMostRanks - 1) / kMostRanks);     // of workgroups, a range's
+    const int64_t groups = chunks * ((r + kMostRanks - 1) / kMostRanks) * L, most = kCUs * (rows >= kLongRows ? 3 : 1);
     int32_t s = 1;
-    while (2 * s <= kMostRanges && rows >= 2 * s * kRangeRows && 2 * s * groups <= kCUs &&
-           (2 * s * groups) * (2 * s * groups) * L <= int64_t(kCUs) * kCUs)
-        s *= 2;
+    while (2 * s <= kMostRanges && rows >= 2 * s * kRangeRows && 2 * s * groups <= most) s *= 2;
     return s == 2 && L > 1 ? 4 : s;
 }
 
@@ -273,7 +272,8 @@ size_t round16(size_t v) { return (v + 15) / 16 * 16; }
 }  // namespace
 
 size_t lora_grad_workspace(int32_t rows, int32_t m, int32_t n, int32_t r, int32_t L) {
-    const size_t s = splits_of(rows, m, n, r, L, 16 * Mat<uint16_t>::V);
+    const size_t f32 = splits_of(rows, m, n, r, L, ONEXN_F32), bf16 = splits_of(rows, m, n, r, L, ONEXN_BF16);
+    const size_t s = f32 > bf16 ? f32 : bf16;
     return s == 1 ? 0 : round16(s * L * r * (size_t(m) + n) * 4) + round16(s * L * 4);
 }
 
@@ -290,7 +290,7 @@ static void launch_grad(const GradArgs& a, dim3 grid, hipStream_t s) {
 
 void launch_lora_grad(const LoraGradArgs& g, onexn_dtype dt, hipStream_t s) {
     const int32_t cols = 16 * (dt == ONEXN_F32 ? Mat<float>::V : Mat<uint16_t>::V);
-    const int32_t splits = splits_of(g.rows, g.m, g.n, g.r, g.L, cols);
+    const int32_t splits = splits_of(g.rows, g.m, g.n, g.r, g.L, dt);
     GradArgs a{};
     JoinArgs join{};
     float* part = static_cast<float*>(g.workspace);
