@@ -291,7 +291,7 @@ onexn_status onexn_fc_fwd(const int32_t* P_dev, const int32_t* I_dev, const void
  * A row whose id lies outside [0, L) has none: u is 0 and y is base, whatever
  * x holds there (padding, NaN).  Rows may come in any order; in batches of more
  * than 4096 rows those of one adapter should stand together (in any order the
- * result is the same, but slow).
+ * result is the same, but takes up to nine times as long).
  *
  * x_dev:   [rows][m] in xdt, rows x_stride elements apart.
  * A_dev, B_dev: [L][r][m] and [L][r][n] in xdt: both factors hold one row per
@@ -307,7 +307,8 @@ onexn_status onexn_fc_fwd(const int32_t* P_dev, const int32_t* I_dev, const void
  * Arrays are aligned to their elements; strides are at least the width.  Sums
  * are fp32; a bf16 layer's second product takes all 24 bits of u, whatever y's
  * type is.
- * Where x, u or a factor is not finite, the row's results are not.
+ * Where x, u or a factor of a row's adapter is not finite, that row's results
+ * need not be; other rows' are not touched by it.
  * Supported: 1 <= r <= 128, L <= 32767, rows <= 2^26, m and n <= 2^27, r*m and
  *         r*n below 2^31.
  * Errors: NULL, DTYPE, ARG, UNSUPPORTED, HIP (launch failed).  rows == 0 is a

@@ -11,8 +11,9 @@
 // partial sum; whoever needs the norm adds all partial sums in their order, so
 // that every workgroup of the scaling gets the same bits without a launch
 // between the two.  Squares and sums are 64-bit: a square of fp32 neither
-// overflows nor vanishes, and the sum of 2^31 elements keeps 22 bits to spare
-// over fp32.
+// overflows nor vanishes, and with 2^31 elements none passes more than some 160
+// additions (64 of its chunk, as many chunks of its workgroup, the trees and the
+// partial sums): N is off by less than 2^-45 of it before it is rounded to fp32.
 #include <cmath>
 
 #include "conv_common.h"
